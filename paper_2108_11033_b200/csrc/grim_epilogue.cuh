@@ -42,10 +42,15 @@ __device__ __forceinline__ void fma2(float& r0, float& r1, float a0, float a1, f
       : "=f"(r0), "=f"(r1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1), "f"(c0), "f"(c1));
 }
 
-// The smaller of two numbers, NaN if one is.
+// The smaller, the larger of two numbers, NaN if one is.
 __device__ __forceinline__ float min_nan(float a, float b) {
   float y;
   asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
   return y;
 }
 
@@ -179,7 +184,12 @@ __device__ __forceinline__ void act_slopes(int act, const float (&p)[N], float (
       break;
     case GRIM_ACT_SILU:
 #pragma unroll
-      for (int i = 0; i < N; ++i) { float q, k; sigmoid_pair<true>(p[i], q, k); d[i] = q * fmaf(p[i], k, 1.f); }
+      for (int i = 0; i < N; ++i) {
+        // q (1 + c k), c = p but no less than -88.  e = e^-c stays finite there (2^126.96), and from 2^126 on q leaves the range of
+        // 1 / x and is 0: so the slope goes to 0 and does not grow with p.  NaN stays NaN.
+        const float c = max_nan(p[i], -88.f), e = exp2_(c * -kLog2e), q = inverse(1.f + e);
+        d[i] = q * fmaf(c, e * q, 1.f);
+      }
       break;
     case GRIM_ACT_GELU:
       if constexpr (N >= 8) {

@@ -1,0 +1,63 @@
+"""Epilogues, their gradient and what else stands around the products, far out: at the lowest and the largest numbers, infinities and NaN.
+
+Bounds that do not grow with |p|, u = 2^-24.
+  SiLU's slope, q (1 + c k), e = e^-c, q = 1 / (1 + e), k = e q, c = p but no less than -88.  e is off by (|c| + 5) u of itself (the exponent's
+  rounding, 2 ulp of the power), and of q by at most the share e / (1 + e) of that, 3 u more from the sum and the reciprocal (1 ulp).
+  c >= 0: |c| e <= 0.37, so q is within 8.4 u; c k <= 0.28 and within 4.6 u; the slope, at most 1.28 times 10.4 u and 4.6 u: 18 u.
+  c < 0: q <= e^-|c| and within (|c| + 8) u, e^-|c| (1 + |c|) (|c| + 10) <= 10; k's share, q |c| times what e leaves in e / (1 + e) and
+  3 u, below 3 u: 13 u.  24 u for both, and below -88 less than 89 e^-88 < 6e-37.
+The sum over N columns in a tree whose longest path is one thread's share: (N / 32 + 32) u of the sum of magnitudes.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer_oracle as lo
+from test_gpu_layers import B, BF16, F32, U, close, dev, num  # noqa: F401  (B: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+LOWEST = {F32: float(np.finfo(np.float32).min), BF16: -3.3895313892515355e38}
+FAR = [0.0, -0.0, 1e-38, -1e-38, 1.0, -1.0, 79.5, -79.5, 80.5, -80.5, 87.0, -87.0, 88.0, -88.0, 88.5, -88.5, 100.0, -100.0, 1e4, -1e4, 1e19, -1e19, 1e20,
+       -1e20, 1e28, -1e28, 1e30, -1e30, 1e35, -1e35]
+
+
+def slope_case(B, act, dtype, N, slope_bound, limits):
+    """Rows whose P holds one far value in some places among ordinary ones; limits: the slope at -infinity and infinity (NaN
+    where the formula is 0 times infinity)."""
+    values = FAR + [LOWEST[dtype], -LOWEST[dtype]]
+    M = len(values) + 3
+    g = np.random.default_rng(N)
+    P, DY = dev(2 * g.normal(size=(M, N)), dtype), dev(g.normal(size=(M, N)), dtype)
+    at = sorted({0, 5 % N, N // 2, N - 1})
+    for r, v in enumerate(values + [-np.inf, np.inf, np.nan]):
+        P[r, at] = v
+    p, dy = num(P), num(DY)
+    finite = np.arange(M) < len(values)
+    want = dy.copy()
+    want[finite] *= lo.act_grad(act, p[finite])
+    rest = np.setdiff1d(np.arange(N), at)
+    for r, v in ((M - 3, limits[0]), (M - 2, limits[1]), (M - 1, np.nan)):
+        want[r, rest] *= lo.act_grad(act, p[r, rest])
+        want[r, at] *= v
+    bound = slope_bound * np.abs(dy)
+    for out in ("new", "dY", "pre", None):
+        dY, pre = DY.clone(), P.clone()
+        dP = {"new": torch.empty_like(DY), "dY": dY, "pre": pre, None: None}[out]
+        db = torch.empty(M, device="cuda")
+        B.grim_epilogue_grad(dY, dP, lo.ACTS.index(act), pre, db)
+        whole = ~np.isnan(want)
+        rows = whole.all(1)
+        if dP is not None:
+            got = num(dP)
+            assert np.array_equal(np.isnan(got), ~whole)
+            close(got[whole], want[whole], bound[whole], dtype, "dP")
+        s = num(db)
+        assert np.array_equal(np.isnan(s), ~rows)
+        close(s[rows], want[rows].sum(1), bound[rows].sum(1) + (N / 32 + 32) * U * np.abs(want[rows]).sum(1), F32, "dbias")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N", [1, 7, 333, 4100])
+def test_slope_of_silu_far_out(B, dtype, N):  # noqa: F811
+    slope_case(B, "silu", dtype, N, 24 * U, (0.0, np.nan))
