@@ -221,7 +221,8 @@ grim_status_t grim_bcr_spmm(grim_bcr_t h, const grim_mat_t* X, grim_mat_t* Y, gr
  *   act: see grim_act_t; applied in fp32.
  *   residual: M x N in Y's type, or NULL.  It may be Y itself (same memory and stride); a partial overlap is not allowed.
  *   pre: M x N in Y's type, receives W * X + bias (what grim_epilogue_grad asks for), or NULL; overlaps nothing.
- * Everything is fp32 until one rounding to each output's type.  Rows kept by no block are act(bias) + residual.
+ * Everything is fp32 until one rounding to each output's type.  Rows kept by no block are act(bias) + residual.  SILU, GELU and
+ * GELU_TANH of -infinity are NaN (0 times infinity); SIGMOID is never below 1.8e-35.
  */
 typedef enum {
   GRIM_ACT_NONE = 0,
@@ -247,7 +248,8 @@ grim_status_t grim_bcr_linear_ex(grim_bcr_t h, const grim_mat_t* X, const grim_e
  * the residual's gradient is dY itself, and X's is W^T dP: grim_bcr_spmm with the handle that grim_bcr_transpose makes.  dY, pre
  * and dP: [M x N] of one type, fp32 or bf16.  pre may be NULL for GRIM_ACT_NONE; dP may be dY or pre, or NULL where only
  * the sums are wanted; dbias_dev: M fp32 DEVICE values or NULL (not both).  One launch, asynchronous, allocates nothing.
- * Weights have no gradient here: a handle's values are constants. */
+ * act' of the lowest and of the largest numbers is 0 or 1; where pre is infinite, GELU's, and SILU's at +infinity, are NaN, the others
+ * their limits.  Weights have no gradient here: a handle's values are constants. */
 grim_status_t grim_epilogue_grad(const grim_mat_t* dY, const grim_mat_t* pre, grim_act_t act, grim_mat_t* dP, float* dbias_dev,
                                  grim_stream_t stream);
 

@@ -208,8 +208,9 @@ __device__ __forceinline__ void act_slopes(int act, const float (&p)[N], float (
     case GRIM_ACT_GELU_TANH:
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const float s = p[i] * p[i], t = tanh_(kSqrt2OverPi * fmaf(kGeluCubic * s, p[i], p[i]));
-        d[i] = 0.5f * (1.f + t) + 0.5f * p[i] * fmaf(-t, t, 1.f) * kSqrt2OverPi * fmaf(3.f * kGeluCubic, s, 1.f);
+        // (1 + t) / 2 + (1 - t^2) (3 a / 2 - r), a = r + 0.044715 r c^2, r = sqrt(2 / pi) c: little cancels, |a| >= |r|.  Beyond 16 the slope is 0 or 1: c is p kept within it, so that 1 - t^2 = 0 never meets an a that is infinite.
+        const float c = max_nan(min_nan(p[i], 16.f), -16.f), r = kSqrt2OverPi * c, a = fmaf(kGeluCubic * c * c, r, r), t = tanh_(a);
+        d[i] = fmaf(fmaf(-t, t, 1.f), fmaf(1.5f, a, -r), fmaf(0.5f, t, 0.5f));
       }
       break;
     case GRIM_ACT_SIGMOID:

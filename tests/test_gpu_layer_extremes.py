@@ -6,6 +6,12 @@ Bounds that do not grow with |p|, u = 2^-24.
   c >= 0: |c| e <= 0.37, so q is within 8.4 u; c k <= 0.28 and within 4.6 u; the slope, at most 1.28 times 10.4 u and 4.6 u: 18 u.
   c < 0: q <= e^-|c| and within (|c| + 8) u, e^-|c| (1 + |c|) (|c| + 10) <= 10; k's share, q |c| times what e leaves in e / (1 + e) and
   3 u, below 3 u: 13 u.  24 u for both, and below -88 less than 89 e^-88 < 6e-37.
+  GELU_TANH's slope, (1 + t) / 2 + A (1 - t^2), t = tanh(a), r = sqrt(2 / pi) c, a = r + 0.044715 r c^2, A = 3 a / 2 - r, c = p within 16 of
+  zero.  1 - t^2 is off by 2 |t| times t's error and by one rounding.  Up to a = 0.6 t is within 8 u of itself and A <= 0.33: 5.2 u and a
+  third of that.  From there on t is off by half a step, u / 2, and by (1 - t) (2 a + 8) u, and a's four roundings add (1 - t^2) a 4 u, which
+  together stay below 6 u and below u / 2 + 0.1 u from c = 3 on, while A is 0.5, 2.7, 9.7 at c = 1, 3, 5.2.  Beyond 5.2 t is 1.  That is 11 u
+  at c = 5.2, where 1 - t^2 is nothing, and 4 u at c = 1.  A is within 15 u of itself, and A (1 - t^2) <= 0.3: 5 u.  The first summand is
+  within 4 u, the last sum, of at most 1.13, rounds once more: 24 u.
 The sum over N columns in a tree whose longest path is one thread's share: (N / 32 + 32) u of the sum of magnitudes.
 """
 import numpy as np
@@ -61,3 +67,9 @@ def slope_case(B, act, dtype, N, slope_bound, limits):
 @pytest.mark.parametrize("N", [1, 7, 333, 4100])
 def test_slope_of_silu_far_out(B, dtype, N):  # noqa: F811
     slope_case(B, "silu", dtype, N, 24 * U, (0.0, np.nan))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N", [1, 7, 333, 4100])
+def test_slope_of_gelu_tanh_far_out(B, dtype, N):  # noqa: F811
+    slope_case(B, "gelu_tanh", dtype, N, 24 * U, (0.0, 1.0))
