@@ -54,7 +54,7 @@ typedef struct CUstream_st* grim_stream_t;
 typedef struct grim_bcr* grim_bcr_t; /* a packed BCR weight matrix */
 typedef struct grim_gru* grim_gru_t; /* a multi-layer GRU built from packed matrices */
 
-/* A dense row-major matrix in DEVICE memory: element (r, c) is at ptr[r * ld + c]. */
+/* A dense row-major matrix in DEVICE memory: element (r, c) is at ptr[r * ld + c]; ptr lies on a boundary of its elements. */
 typedef struct {
   void* ptr;
   int64_t rows, cols, ld;

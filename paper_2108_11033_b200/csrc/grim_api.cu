@@ -10,8 +10,11 @@ using namespace grim;
 
 namespace {
 
+// Kernels read and write whole elements.
+bool on_element(const grim_mat_t* m) { return reinterpret_cast<uintptr_t>(m->ptr) % (m->dtype == GRIM_F32 ? 4 : 2) == 0; }
+
 grim_status_t check_mats(const grim_bcr* h, const grim_mat_t* X, const grim_mat_t* Y) {
-  if (!h || !X || !Y || !X->ptr || !Y->ptr) return GRIM_ERR_INVALID_ARG;
+  if (!h || !X || !Y || !X->ptr || !Y->ptr || !on_element(X) || !on_element(Y)) return GRIM_ERR_INVALID_ARG;
   if (h->device < 0) return GRIM_ERR_INVALID_ARG;
   if (X->rows != h->K || Y->rows != h->M || X->cols != Y->cols || X->cols <= 0) return GRIM_ERR_SHAPE;
   if (X->ld < X->cols || Y->ld < Y->cols) return GRIM_ERR_SHAPE;
@@ -215,7 +218,7 @@ extern "C" grim_status_t grim_bcr_linear(grim_bcr_t h, const grim_mat_t* X, cons
 
 extern "C" grim_status_t grim_bcr_linear_ex(grim_bcr_t h, const grim_mat_t* X, const grim_epilogue_t* e, grim_mat_t* Y, const grim_tune_t* tune,
                                             grim_stream_t stream) {
-  if (!e) return GRIM_ERR_INVALID_ARG;
+  if (!e || reinterpret_cast<uintptr_t>(e->bias_dev) % 4 != 0) return GRIM_ERR_INVALID_ARG;
   grim_status_t st = check_mats(h, X, Y);
   if (st != GRIM_OK) return st;
   if ((int)e->act < GRIM_ACT_NONE || (int)e->act > GRIM_ACT_TANH) return GRIM_ERR_INVALID_ARG;
@@ -227,7 +230,7 @@ extern "C" grim_status_t grim_bcr_linear_ex(grim_bcr_t h, const grim_mat_t* X, c
   f.e.on = e->act != GRIM_ACT_NONE || e->residual || e->pre;
   for (const grim_mat_t* m : {e->residual, static_cast<const grim_mat_t*>(e->pre)}) {
     if (!m) continue;
-    if (!m->ptr || reinterpret_cast<uintptr_t>(m->ptr) % (m->dtype == GRIM_F32 ? 4 : 2) != 0) return GRIM_ERR_INVALID_ARG;
+    if (!m->ptr || !on_element(m)) return GRIM_ERR_INVALID_ARG;
     if (m->rows != Y->rows || m->cols != Y->cols || m->ld < m->cols) return GRIM_ERR_SHAPE;
     if (m->dtype != Y->dtype) return GRIM_ERR_DTYPE;
   }

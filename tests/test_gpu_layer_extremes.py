@@ -14,6 +14,8 @@ Bounds that do not grow with |p|, u = 2^-24.
   within 4 u, the last sum, of at most 1.13, rounds once more: 24 u.
 The sum over N columns in a tree whose longest path is one thread's share: (N / 32 + 32) u of the sum of magnitudes.
 """
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -73,3 +75,29 @@ def test_slope_of_silu_far_out(B, dtype, N):  # noqa: F811
 @pytest.mark.parametrize("N", [1, 7, 333, 4100])
 def test_slope_of_gelu_tanh_far_out(B, dtype, N):  # noqa: F811
     slope_case(B, "gelu_tanh", dtype, N, 24 * U, (0.0, 1.0))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_products_refuse_operands_between_elements(B, bf16):  # noqa: F811
+    """Refused on the host: nothing is launched, nothing written."""
+    M, K, N, dt, esz = 32, 16, 24, BF16 if bf16 else F32, 2 if bf16 else 4
+    h = B.grim_bcr_pack(np.ones((M, K), np.float32), np.ones((M, K), np.uint8), 4, 16, int(bf16), 0)
+    buf = {k: torch.full((M * N + 8,), 3.0, device="cuda", dtype=dt) for k in "XYRP"}
+    bias = torch.zeros(M + 2, device="cuda")
+    torch.cuda.synchronize()
+    before = B.grim_launch_count()
+    for off in range(1, esz):
+        for which in ("X", "Y", "R", "P", "bias"):
+            mat = {k: B.grim_mat_t(t.data_ptr() + (off if k == which else 0), K if k == "X" else M, N, N, int(bf16)) for k, t in buf.items()}
+            x, y, r, p = (C.byref(mat[k]) for k in "XYRP")
+            e = B.grim_epilogue_t(bias.data_ptr() + (off if which == "bias" else 0), B.GRIM_ACT_SILU, C.pointer(mat["R"]), C.pointer(mat["P"]))
+            tune = B.grim_tune_t()
+            got = [B.lib.grim_bcr_linear(h, x, C.byref(e), y, None), B.lib.grim_bcr_linear_ex(h, x, C.byref(e), y, C.byref(tune), None)]
+            if which in "XY":
+                got += [B.lib.grim_bcr_spmm(h, x, y, None), B.lib.grim_bcr_spmm_ex(h, x, y, C.byref(tune), None)]
+            assert got == [B.GRIM_ERR_INVALID_ARG] * len(got), (which, off, got)
+    assert B.grim_launch_count() == before
+    torch.cuda.synchronize()
+    assert all((t == 3.0).all() for t in buf.values())
+    assert B.grim_bcr_status(h) == B.GRIM_OK
+    B.grim_bcr_destroy(h)
