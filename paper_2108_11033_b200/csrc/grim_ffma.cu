@@ -128,7 +128,9 @@ __device__ __forceinline__ float ld_x1(const __nv_bfloat16* slab, unsigned col, 
 // halves of a warp split the kept columns of a chunk between them (lanes 0-15 the first four, lanes 16-31 the
 // other four; their sums meet in one shuffle at the end).  The kept values then stream through shared memory once
 // and each costs a quarter of a broadcast load and one FMA per lane - no per-lane gathers from global memory.
-template <int BH, int BPW, int CW, typename XT, int MODE>
+// EPI: activation, residual and values before the activation too (grim_bcr_linear); products without them keep a kernel without them
+// (sharing one cost the narrow tile up to 4 %: 8 x 32 blocks, 4096^2, N = 16, two bands per warp: 31.4 -> 32.5 us).
+template <int BH, int BPW, int CW, typename XT, int MODE, bool EPI>
 __global__ void __launch_bounds__(kFThreads, CW == 0 ? 2 : 1) bcr_ffma_kernel(const __grid_constant__ CUtensorMap tmX, const FParams p) {
   constexpr bool NARROW = CW == 0;
   constexpr int NS = NARROW ? kNarrowStages : kStages, AH = NARROW ? kNarrowAhead : kAhead;  // ring slots, stages in flight
@@ -447,7 +449,7 @@ __global__ void __launch_bounds__(kFThreads, CW == 0 ? 2 : 1) bcr_ffma_kernel(co
       t[e] += bias;
       if (a.relu) t[e] = fmaxf(t[e], 0.f);
     }
-    if (a.e.on) epilogue4(a.e, a.y_dtype, t, row, q, (int)min(a.ncols - q, (int64_t)4));
+    if constexpr (EPI) epilogue4(a.e, a.y_dtype, t, row, q, (int)min(a.ncols - q, (int64_t)4));
     int64_t off0;
     bool contiguous;
     if (a.conv) {
@@ -567,7 +569,7 @@ __global__ void __launch_bounds__(kFThreads, CW == 0 ? 2 : 1) bcr_ffma_kernel(co
         const int64_t off = row * rstride + qbase;
         t += a.bias ? __ldg(a.bias + row) : 0.f;
         if (a.relu) t = fmaxf(t, 0.f);
-        if (a.e.on) t = epilogue(a.e, a.y_dtype, t, row, q);
+        if constexpr (EPI) t = epilogue(a.e, a.y_dtype, t, row, q);
         if (a.y_dtype == GRIM_F32) static_cast<float*>(a.Y)[off] = t;
         else static_cast<__nv_bfloat16*>(a.Y)[off] = __float2bfloat16_rn(t);
       }
@@ -622,7 +624,7 @@ bool tma_eligible(const SpmmArgs& a) {
 
 template <int BH, int BPW, int CW, typename XT, int MODE>
 cudaError_t launch_variant(const CUtensorMap& tm, const FParams& p, size_t smem, dim3 grid, cudaStream_t s) {
-  auto kern = bcr_ffma_kernel<BH, BPW, CW, XT, MODE>;
+  auto kern = p.a.e.on ? bcr_ffma_kernel<BH, BPW, CW, XT, MODE, true> : bcr_ffma_kernel<BH, BPW, CW, XT, MODE, false>;
   cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};

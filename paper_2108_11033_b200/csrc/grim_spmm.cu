@@ -15,6 +15,7 @@
 #include <cuda_bf16.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "grim_epilogue.cuh"
 #include <mutex>
@@ -131,7 +132,9 @@ __device__ __forceinline__ float4 load_unit(const KParams& p, int64_t k, int64_t
   }
 }
 
-template <int BH, int BPW, int NQL, typename VT, bool CONV>
+// EPI: activation, residual and values before the activation too (grim_bcr_linear); products without them keep a kernel without them
+// (sharing one cost them up to 7 %: 16 x 64 blocks, 2048^2, N = 512, tiles of 16 columns: 152 -> 162 us).
+template <int BH, int BPW, int NQL, typename VT, bool CONV, bool EPI>
 __global__ void __launch_bounds__(kThreads) bcr_spmm_kernel(const KParams p) {
   constexpr int TN = NQL * 4;
   constexpr int KQ = 32 / NQL;
@@ -298,7 +301,7 @@ __global__ void __launch_bounds__(kThreads) bcr_spmm_kernel(const KParams p) {
         t[e] += bias;
         if (a.relu) t[e] = fmaxf(t[e], 0.f);
       }
-      if (!CONV && a.e.on) epilogue4(a.e, a.y_dtype, t, row, q, (int)min(a.ncols - q, (int64_t)4));
+      if constexpr (EPI) epilogue4(a.e, a.y_dtype, t, row, q, (int)min(a.ncols - q, (int64_t)4));
       int64_t off0;
       bool contiguous;
       if (CONV) {
@@ -366,6 +369,9 @@ struct SkinnyParams {
   void* Y;
   int64_t ldx, ldy;
   int N, nbr, M, bh, wpb, y_dtype, vec_ok;
+};
+// with what follows the product (grim_bcr_linear); products without it keep a kernel without it
+struct SkinnyParamsFollow : SkinnyParams {
   const float* bias;
   Epilogue e;
 };
@@ -394,8 +400,9 @@ __device__ __forceinline__ void load_x_row(const SkinnyParams& p, uint32_t col, 
   }
 }
 
-template <int BH, int NQ, int U, typename VT, typename XT>
-__global__ void __launch_bounds__(kThreads) bcr_skinny_kernel(const SkinnyParams p) {
+template <int BH, int NQ, int U, typename VT, typename XT, typename P>
+__global__ void __launch_bounds__(kThreads) bcr_skinny_kernel(const P p) {
+  constexpr bool FOLLOW = std::is_same<P, SkinnyParamsFollow>::value;
   __shared__ float part[kWarps][BH][NQ];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int wpb = p.wpb, bpc = kWarps / wpb;
@@ -488,8 +495,10 @@ __global__ void __launch_bounds__(kThreads) bcr_skinny_kernel(const SkinnyParams
       if (r >= p.bh || row >= p.M || q0 + q >= p.N) continue;
       float s = 0.f;
       for (int w = 0; w < wpb; ++w) s += part[bi * wpb + w][r][q];
-      if (p.bias) s += __ldg(p.bias + row);
-      if (p.e.on) s = epilogue(p.e, p.y_dtype, s, row, q0 + q);
+      if constexpr (FOLLOW) {
+        if (p.bias) s += __ldg(p.bias + row);
+        s = epilogue(p.e, p.y_dtype, s, row, q0 + q);
+      }
       if (p.y_dtype == GRIM_F32) static_cast<float*>(p.Y)[row * p.ldy + q0 + q] = s;
       else static_cast<__nv_bfloat16*>(p.Y)[row * p.ldy + q0 + q] = __float2bfloat16_rn(s);
     }
@@ -502,7 +511,7 @@ cudaError_t launch_one(const KParams& p, cudaStream_t s) {
   KParams q = p;
   q.blob_stride = (p.blob_stride + 15u) & ~15u;
   const size_t smem = (size_t)2 * p.bw * TN * 4 + (size_t)2 * q.blob_stride;
-  auto kern = bcr_spmm_kernel<BH, BPW, NQL, VT, CONV>;
+  auto kern = !CONV && p.a.e.on ? bcr_spmm_kernel<BH, BPW, NQL, VT, CONV, !CONV> : bcr_spmm_kernel<BH, BPW, NQL, VT, CONV, false>;
   if (smem > 48 * 1024) {
     cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
     if (e != cudaSuccess) return e;
@@ -560,21 +569,21 @@ grim_status_t launch_spmm(const grim_bcr* h, const SpmmArgs& a, cudaStream_t s) 
 
 namespace {
 
-template <int BH, typename VT, typename XT>
-cudaError_t launch_skinny_nq(const SkinnyParams& p, int nq, dim3 grid, cudaStream_t s) {
+template <int BH, typename VT, typename XT, typename P>
+cudaError_t launch_skinny_nq(const P& p, int nq, dim3 grid, cudaStream_t s) {
   switch (nq) {
-    case 1: bcr_skinny_kernel<BH, 1, 4, VT, XT><<<grid, kThreads, 0, s>>>(p); break;
-    case 4: bcr_skinny_kernel<BH, 4, 4, VT, XT><<<grid, kThreads, 0, s>>>(p); break;
-    case 8: bcr_skinny_kernel<BH, 8, 2, VT, XT><<<grid, kThreads, 0, s>>>(p); break;
+    case 1: bcr_skinny_kernel<BH, 1, 4, VT, XT, P><<<grid, kThreads, 0, s>>>(p); break;
+    case 4: bcr_skinny_kernel<BH, 4, 4, VT, XT, P><<<grid, kThreads, 0, s>>>(p); break;
+    case 8: bcr_skinny_kernel<BH, 8, 2, VT, XT, P><<<grid, kThreads, 0, s>>>(p); break;
     default:
       if (BH > 8) return cudaErrorInvalidValue;
-      bcr_skinny_kernel<(BH <= 8 ? BH : 8), 16, 2, VT, XT><<<grid, kThreads, 0, s>>>(p);
+      bcr_skinny_kernel<(BH <= 8 ? BH : 8), 16, 2, VT, XT, P><<<grid, kThreads, 0, s>>>(p);
   }
   return cudaGetLastError();
 }
 
-template <typename VT, typename XT>
-cudaError_t launch_skinny_bh(const SkinnyParams& p, int BHc, int nq, dim3 grid, cudaStream_t s) {
+template <typename VT, typename XT, typename P>
+cudaError_t launch_skinny_bh(const P& p, int BHc, int nq, dim3 grid, cudaStream_t s) {
   if (BHc == 4) return launch_skinny_nq<4, VT, XT>(p, nq, grid, s);
   if (BHc == 8) return launch_skinny_nq<8, VT, XT>(p, nq, grid, s);
   return launch_skinny_nq<16, VT, XT>(p, nq, grid, s);
@@ -596,7 +605,7 @@ grim_status_t launch_skinny(const grim_bcr* h, const void* X, int x_dtype, int64
   const int64_t want_warps = (int64_t)sm_count(h->device) * 20;
   while (wpb < 8 && (int64_t)nbr * passes * wpb < want_warps && (int64_t)nbr * wpb * 8 <= h->nchunks) wpb *= 2;
   const int bpc = kWarps / wpb;
-  SkinnyParams p;
+  SkinnyParamsFollow p;
   p.band_ptr = h->d_gemv_band_ptr; p.chunks = h->d_chunks; p.colwords = h->d_colwords; p.vals = h->d_gemv_vals;
   p.band_order = h->d_band_order; p.X = X; p.Y = Y; p.ldx = ldx; p.ldy = ldy;
   p.N = (int)N; p.nbr = nbr; p.M = (int)h->M; p.bh = h->bh; p.wpb = wpb; p.y_dtype = y_dtype;
@@ -604,8 +613,10 @@ grim_status_t launch_skinny(const grim_bcr* h, const void* X, int x_dtype, int64
   const int esz = x_dtype == GRIM_F32 ? 4 : 2;
   p.vec_ok = (N % nq == 0) && ldx % 4 == 0 && (reinterpret_cast<uintptr_t>(X) % (4 * esz)) == 0;
   dim3 grid((unsigned)((nbr + bpc - 1) / bpc), (unsigned)passes);
-  cudaError_t e = h->dtype == GRIM_F32 ? launch_skinny_bh<float, float>(p, BHc, nq, grid, s)
-                                       : launch_skinny_bh<__nv_bfloat16, __nv_bfloat16>(p, BHc, nq, grid, s);
+  auto launch = [&](const auto& q) {
+    return h->dtype == GRIM_F32 ? launch_skinny_bh<float, float>(q, BHc, nq, grid, s) : launch_skinny_bh<__nv_bfloat16, __nv_bfloat16>(q, BHc, nq, grid, s);
+  };
+  const cudaError_t e = p.bias || p.e.on ? launch(p) : launch(static_cast<const SkinnyParams&>(p));
   count_launch();
   return e == cudaSuccess ? GRIM_OK : GRIM_ERR_CUDA;
 }
