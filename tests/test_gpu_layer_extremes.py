@@ -21,7 +21,8 @@ import pytest
 import torch
 
 from oracle import layer_oracle as lo
-from test_gpu_layers import B, BF16, F32, U, close, dev, num  # noqa: F401  (B: the fixture)
+from test_gpu_layers import B, BF16, F32, KERNELS, U, close, dev, num  # noqa: F401  (B: the fixture)
+from workloads import generators as gen
 
 pytestmark = pytest.mark.gpu
 
@@ -32,7 +33,7 @@ FAR = [0.0, -0.0, 1e-38, -1e-38, 1.0, -1.0, 79.5, -79.5, 80.5, -80.5, 87.0, -87.
 
 def slope_case(B, act, dtype, N, slope_bound, limits):
     """Rows whose P holds one far value in some places among ordinary ones; limits: the slope at -infinity and infinity (NaN
-    where the formula is 0 times infinity)."""
+    where the formula is 0 times infinity), and at NaN where that is a number."""
     values = FAR + [LOWEST[dtype], -LOWEST[dtype]]
     M = len(values) + 3
     g = np.random.default_rng(N)
@@ -45,7 +46,7 @@ def slope_case(B, act, dtype, N, slope_bound, limits):
     want = dy.copy()
     want[finite] *= lo.act_grad(act, p[finite])
     rest = np.setdiff1d(np.arange(N), at)
-    for r, v in ((M - 3, limits[0]), (M - 2, limits[1]), (M - 1, np.nan)):
+    for r, v in zip((M - 3, M - 2, M - 1), (*limits, np.nan)):
         want[r, rest] *= lo.act_grad(act, p[r, rest])
         want[r, at] *= v
     bound = slope_bound * np.abs(dy)
@@ -101,3 +102,45 @@ def test_products_refuse_operands_between_elements(B, bf16):  # noqa: F811
     assert all((t == 3.0).all() for t in buf.values())
     assert B.grim_bcr_status(h) == B.GRIM_OK
     B.grim_bcr_destroy(h)
+
+
+@pytest.mark.parametrize("act", lo.ACTS)
+@pytest.mark.parametrize("kernel", KERNELS, ids=[k[0] for k in KERNELS])
+def test_activations_far_out_in_every_kernel(B, kernel, act):  # noqa: F811
+    """X = 0, so that p is the bias: y is within 8 u of itself and 32 u, whatever p; sigmoids stop at 1.8e-35."""
+    _, size, choice = kernel
+    s = dict(bf16=False, **size) if "bf16" not in size else size
+    M, K, N, bf16 = s["M"], s["K"], s["N"], s["bf16"]
+    W = gen.dense_weight(M, K, seed=21)
+    h = B.grim_bcr_pack(W, gen.bcr_mask(M, K, s["bh"], s["bw"], compression=s["rate"], dist="uniform", seed=22, stream=3), s["bh"], s["bw"], int(bf16), 0)
+    if bf16:
+        B.grim_bcr_reserve(h, N)
+    X = torch.zeros(K, N, device="cuda", dtype=BF16 if bf16 else F32)
+    for yt in ((BF16, F32) if bf16 else (F32,)):
+        values = FAR + [LOWEST[yt], -LOWEST[yt], np.inf, -np.inf, np.nan]
+        b = np.resize(np.asarray(values, np.float32), M)
+        R = torch.randn(M, N, device="cuda").to(yt)
+        Y, P = torch.empty(M, N, device="cuda", dtype=yt), torch.empty(M, N, device="cuda", dtype=yt)
+        B.grim_bcr_linear(h, X, Y, dev(b), lo.ACTS.index(act), R, P, **choice)
+        with np.errstate(invalid="ignore", over="ignore"):
+            y = lo.act(act, b.astype(np.float64))[:, None]
+        if act == "relu":
+            y = np.where(np.isnan(b[:, None]), np.nan, y)
+        want = y + num(R)
+        got = num(Y)
+        sure = np.isfinite(want)
+        assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[np.isinf(want)], want[np.isinf(want)])
+        close(got[sure], want[sure], (32 * U + 8 * U * np.abs(want) + 1e-34)[sure], yt, "Y")
+        assert torch.equal(torch.nan_to_num(P), torch.nan_to_num(dev(b)[:, None].expand(M, N).to(yt))) and torch.equal(torch.isnan(P), torch.isnan(dev(b))[:, None].expand(M, N))
+    assert B.grim_bcr_status(h) == B.GRIM_OK
+    B.grim_bcr_destroy(h)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "sigmoid", "tanh"])
+def test_other_slopes_far_out(B, act, dtype):  # noqa: F811
+    """GELU's slope, Phi(p) + p e / sqrt(2 pi), e = e^(-p^2 / 2): e's exponent rounds by up to 1.5 p^2 / 2 u and its power by 4 u, and
+    p e <= 0.61, p^3 e <= 1.16, so the second summand is within 0.4 (0.75 * 1.16 + 6 * 0.61) u < 2 u; Phi is within 4.2 u; one fma: 10 u.
+    sigmoid's, q k <= 1/4, each within (|p| + 9) u of itself, |p| q k <= 0.23: 5 u; tanh's, 1 - t^2: 16 u and a rounding.  24 u for all."""
+    for N in (1, 7, 333, 4100):
+        slope_case(B, act, dtype, N, 24 * U, {"gelu": (np.nan, np.nan), "none": (1.0, 1.0, 1.0), "relu": (0.0, 1.0, 0.0)}.get(act, (0.0, 0.0)))
