@@ -3,13 +3,22 @@ its gradient, and the gated linear recurrence with its gradient, from their defi
 
 Every recurrence also returns how large the numbers behind a result were and how far a 32-bit evaluation in any order may be from
 it, so that the tests' tolerances follow from the arithmetic.  With u = 2^-24 (half a step of fp32):
-  e = exp(-|g|) as 2^(-|g| log2 e): the product rounds the exponent by up to |g| u, the power is within 2 ulp = 4 u: (|g| + 5) u;
-  of sigmoid(g) and its complement the larger, 1 / (1 + e), is within 3 u and what e brings, at most its own share
-  e / (1 + e) of it; the smaller, e / (1 + e), within (|g| + 9) u;
-  tanh(v) is within 8 u, the candidate's factor (1 - a) n within 10 u more than 1 - a;
-  a step h = a h + w then adds (off_a + 4 u) |a h| + (off_k + 10 u) |w| to what the state before it was off by, times a;
-  evaluated as a tree (eight columns of a lane, 5 levels of a warp, up to 8 warps and 8 blocks one after the other, rounds), a
-  term passes through at most 40 more roundings of partial results that are no larger than the sum of magnitudes: 40 u M.
+  e = exp(-g) as 2^(-g log2 e): the product rounds by u, the constant by 0.23 u, the power is within 2 ulp = 4 u: x = (1.23 |g| + 4) u of itself;
+  sigmoid(g) = a = 1 / (1 + e): the sum's rounding and the reciprocal (1 ulp) are 3 u, and of x it has the share e / (1 + e);
+  1 - a = k = e a: one product more, 4 u, and of x, which e and a have the other way round, what is left, 1 / (1 + e).
+  So for g >= 0 a is within 3 u + x sigmoid(-|g|) and k within 4 u + x; for g < 0 a is within 3 u + x and k within 4 u + x sigmoid(-|g|).
+  (The kernels stop e at 2^115 or e^80, so that a below 2.4e-35 is not told apart; tests that use these bounds keep |g| below 79.)
+  tanh(v) is within 8 u, the candidate's factor (1 - a) n within 9 u more than 1 - a;
+  a step h = a h + w then adds (off_a + 4 u) |a h| + (off_k + 10 u) |w| to what the state before it was off by, times a: the kernels round a
+  column's share of a product of a's once, its sum once when columns are composed and once when the states are worked out.
+  Composed as a tree, a term passes two roundings (a product of a's and a sum) on each of five levels of a warp, three of the warps of a
+  block and three of the blocks of a cluster, and one when what comes in is applied to block, warp and lane: 25, and no partial
+  result is larger than the sum of magnitudes M: 40 u M.  (A round's end rounds once more, behind 256 columns or more.)
+
+Activations, y = act(p): SiLU is p q, q = 1 / (1 + e) with e = exp(-p), which is large where p < 0: q is within (1.23 |p| + 7) u of itself,
+and q <= e^-|p|, so y is off by |p| e^-|p| (1.23 |p| + 8) u < 4 u there, and by less than 8 u |p| where p >= 0.  sigmoid is within 8 u, tanh within 8 u.
+GELU's tail Q(|p|) = e t P(t), e = 2^(-p^2 / 2 log2 e): square, product and constant round by 2.23 u, so the tail is within
+(1.2 p^2 + 10.5) u of itself, Q <= 1/2 and p^2 Q <= 0.17: 5.4 u of 1.  Their products with p stay within 32 u (1 + |p|).
 """
 from __future__ import annotations
 
@@ -72,9 +81,9 @@ def gates_off(mode, G):
     """Bounds for a and 1 - a, relative."""
     if mode == "decay":
         return np.zeros_like(G), np.zeros_like(G)
-    small = (np.abs(G) + 9) * U
-    big = (3 + (np.abs(G) + 5) * sigmoid(-np.abs(G))) * U
-    return np.where(G >= 0, big, small), np.where(G >= 0, small, big)
+    x = 1.23 * np.abs(G) + 4
+    share = x * sigmoid(-np.abs(G))
+    return np.where(G >= 0, 3 + share, 3 + x) * U, np.where(G >= 0, 4 + x, 4 + share) * U
 
 
 def glr_seq(mode, G, V, starts=None, h0=None):

@@ -1,11 +1,11 @@
 """Epilogues, their gradient and what else stands around the products, far out: at the lowest and the largest numbers, infinities and NaN.
 
 Bounds that do not grow with |p|, u = 2^-24.
-  SiLU's slope, q (1 + c k), e = e^-c, q = 1 / (1 + e), k = e q, c = p but no less than -88.  e is off by (|c| + 5) u of itself (the exponent's
-  rounding, 2 ulp of the power), and of q by at most the share e / (1 + e) of that, 3 u more from the sum and the reciprocal (1 ulp).
-  c >= 0: |c| e <= 0.37, so q is within 8.4 u; c k <= 0.28 and within 4.6 u; the slope, at most 1.28 times 10.4 u and 4.6 u: 18 u.
-  c < 0: q <= e^-|c| and within (|c| + 8) u, e^-|c| (1 + |c|) (|c| + 10) <= 10; k's share, q |c| times what e leaves in e / (1 + e) and
-  3 u, below 3 u: 13 u.  24 u for both, and below -88 less than 89 e^-88 < 6e-37.
+  SiLU's slope, q (1 + c k), e = e^-c, q = 1 / (1 + e), k = e q, c = p but no less than -88.  e is off by (1.23 |c| + 4) u of itself (the exponent's
+  rounding and its constant's, 2 ulp of the power), and of q by at most the share e / (1 + e) of that, 3 u more from the sum and the reciprocal (1 ulp).
+  c >= 0: |c| e <= 0.37, so q is within 7.5 u; c k <= 0.28 and within 4.6 u; the slope, at most 1.28 times 9.5 u and 4.6 u: 17 u.
+  c < 0: q <= e^-|c| and within (1.23 |c| + 7) u, e^-|c| (1 + |c|) (1.23 |c| + 10) <= 10.1; k's share, q |c| times what e leaves in e / (1 + e) and
+  3 u, below 3 u: 14 u.  24 u for both, and below -88 less than 89 e^-88 < 6e-37.
   GELU_TANH's slope, (1 + t) / 2 + A (1 - t^2), t = tanh(a), r = sqrt(2 / pi) c, a = r + 0.044715 r c^2, A = 3 a / 2 - r, c = p within 16 of
   zero.  1 - t^2 is off by 2 |t| times t's error and by one rounding.  Up to a = 0.6 t is within 8 u of itself and A <= 0.33: 5.2 u and a
   third of that.  From there on t is off by half a step, u / 2, and by (1 - t) (2 a + 8) u, and a's four roundings add (1 - t^2) a 4 u, which
@@ -139,8 +139,8 @@ def test_activations_far_out_in_every_kernel(B, kernel, act):  # noqa: F811
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("act", ["none", "relu", "gelu", "sigmoid", "tanh"])
 def test_other_slopes_far_out(B, act, dtype):  # noqa: F811
-    """GELU's slope, Phi(p) + p e / sqrt(2 pi), e = e^(-p^2 / 2): e's exponent rounds by up to 1.5 p^2 / 2 u and its power by 4 u, and
-    p e <= 0.61, p^3 e <= 1.16, so the second summand is within 0.4 (0.75 * 1.16 + 6 * 0.61) u < 2 u; Phi is within 4.2 u; one fma: 10 u.
-    sigmoid's, q k <= 1/4, each within (|p| + 9) u of itself, |p| q k <= 0.23: 5 u; tanh's, 1 - t^2: 16 u and a rounding.  24 u for all."""
+    """GELU's slope, Phi(p) + p e / sqrt(2 pi), e = e^(-p^2 / 2): e's exponent rounds by up to 1.2 p^2 u and its power by 4 u, and
+    p e <= 0.61, p^3 e <= 1.16, so the second summand is within 0.4 (1.2 * 1.16 + 6 * 0.61) u < 2.1 u; Phi is within 4.2 u; one fma: 10 u.
+    sigmoid's, q k <= 1/4, each within (1.23 |p| + 8) u of itself, |p| q k <= 0.23: 6 u; tanh's, 1 - t^2: 16 u and a rounding.  24 u for all."""
     for N in (1, 7, 333, 4100):
         slope_case(B, act, dtype, N, 24 * U, {"gelu": (np.nan, np.nan), "none": (1.0, 1.0, 1.0), "relu": (0.0, 1.0, 0.0)}.get(act, (0.0, 0.0)))
