@@ -248,13 +248,15 @@ grim_status_t grim_bcr_linear_ex(grim_bcr_t h, const grim_mat_t* X, const grim_e
  * the residual's gradient is dY itself, and X's is W^T dP: grim_bcr_spmm with the handle that grim_bcr_transpose makes.  dY, pre
  * and dP: [M x N] of one type, fp32 or bf16.  pre may be NULL for GRIM_ACT_NONE; dP may be dY or pre, or NULL where only
  * the sums are wanted; dbias_dev: M fp32 DEVICE values or NULL (not both).  One launch, asynchronous, allocates nothing.
- * act' of the lowest and of the largest numbers is 0 or 1; where pre is infinite, GELU's, and SILU's at +infinity, are NaN, the others
+ * act' of the lowest and of the largest numbers is 0 or 1 (SIGMOID's within 2e-35); where pre is infinite, GELU's, and SILU's at +infinity, are NaN, the others
  * their limits.  Weights have no gradient here: a handle's values are constants. */
 grim_status_t grim_epilogue_grad(const grim_mat_t* dY, const grim_mat_t* pre, grim_act_t act, grim_mat_t* dP, float* dbias_dev,
                                  grim_stream_t stream);
 
 /* The handle of W^T, from a handle's own values (bf16: the rounded ones): blocks of bw x bh, cut to heights of at most 16 that
- * divide bw.  flags as for grim_bcr_pack; a set-up call like it. */
+ * divide bw.  flags as for grim_bcr_pack; a set-up call like it, for the current device.  The kernels for tensor cores take blocks 16, 32 or 64
+ * wide: the handle of a W whose blocks have fewer than 16 rows multiplies on the CUDA cores, and more than 16 columns take 3 to 6 (fp32) or 4 to 24 times
+ * (bf16) as long as with W itself (4096 x 4096).  A bw that no number from 2 to 16 divides gives blocks one row high. */
 grim_status_t grim_bcr_transpose(grim_bcr_t h, uint32_t flags, grim_bcr_t* out);
 
 /* Workspace of the split tensor-core multiply (Section 4.5: the tile plan depends on the problem; bf16 handles with

@@ -2,8 +2,8 @@
 //
 // One pass: two arrays in, one out, and the sums stay in registers until a row is done: warps of a row meet in shared memory, blocks
 // of a row (a cluster, where rows are few) in distributed shared memory.  The order of the additions is fixed: no atomics, the same
-// bits every time.  4096 x 8192: fp32 62 us (62 for its bytes at 6.54 TB/s), memory; bf16 35 us (31) with relu, 39 with gelu, whose
-// slope's instructions fill two thirds of the issue slots.
+// bits every time.  4096 x 8192: fp32 62 us (62 for its bytes at 6.54 TB/s), memory; bf16 35 us (31) with relu, 37 with silu, 39 to 41
+// with gelu, 44 with its tanh form, whose slopes' instructions fill two thirds of the issue slots.
 #include <algorithm>
 
 #include "grim_epilogue.cuh"
@@ -23,11 +23,6 @@ struct GradParams {
 
 template <typename S, int V>
 struct __align__(sizeof(S) * V) Piece { S e[V]; };
-
-__device__ __forceinline__ float widen(float v) { return v; }
-__device__ __forceinline__ float widen(unsigned short v) { return __uint_as_float((uint32_t)v << 16); }
-__device__ __forceinline__ void narrow(float v, float& out) { out = v; }
-__device__ __forceinline__ void narrow(float v, unsigned short& out) { out = __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
 
 // Columns at .. at + V - 1 of a row.
 template <typename S, int V>

@@ -11,8 +11,8 @@
 
 namespace grim {
 
-// The pieces that activations and gates are made of.  2^x and 1/x by the special function unit are within 2 and 1 ulp; products with
-// log2 e round |x| u off the exponent (u = 2^-24, half an ulp), so e^-x is within (|x| + 5) u.
+// The pieces that activations and gates are made of.  2^x and 1/x by the special function unit are within 2 and 1 ulp; the product with
+// log2 e rounds by u (2^-24, half an ulp) and its constant by 0.23 u, so e^-x is within (1.23 |x| + 4) u of itself.
 constexpr float kLog2e = 1.44269504f;
 __device__ __forceinline__ float exp2_(float x) {
   float y;
@@ -55,8 +55,8 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 }
 
 // sigmoid(v) = a = 1 / (1 + e) and 1 - sigmoid(v) = k = e a, e = e^-v: neither is a difference, so both keep their relative precision; e is
-// bounded where a would leave the range of 1 / x.  FAST: e within (|v| + 5) u, which is what values of eight bits deserve; otherwise
-// within 4 u.  (Selecting by v's sign between 1 / (1 + e^-|v|) and its complement costs two selects and a comparison more, on the unit
+// bounded where a would leave the range of 1 / x, so that a is never below 2.4e-35 (1.8e-35 without FAST).  FAST, for values of eight bits:
+// e within (1.23 |v| + 4) u; otherwise within 4 u.  (Selecting by v's sign between 1 / (1 + e^-|v|) and its complement costs two selects and a comparison more, on the unit
 // that a bf16 recurrence keeps busiest: 2048 x 16384 46.5 -> 45.1 us.)
 template <bool FAST = false>
 __device__ __forceinline__ void sigmoid_pair(float v, float& a, float& k) {
@@ -98,7 +98,8 @@ __device__ __forceinline__ float tanh_(float v) {
 }
 
 // e = e^(-v^2 / 2) and the normal distribution's Phi(v).  Its tail is e t P(t), t = 1 / (1 + 0.3 |v|): P of degree 7 fitted for the least
-// largest relative error of the tail on 0 .. 14 (2.5 u; 6.5 u as evaluated), so nothing cancels on either side.
+// largest relative error of the tail on 0 .. 14 (2.5 u; 6.5 u as evaluated, if e is exact), so nothing cancels on either side.  e's exponent is
+// rounded three times, which takes the tail to 11 u of itself up to |v| = 3, 34 u up to 6, 127 u up to 12; of 1 it is 4.2 u.
 __device__ __forceinline__ float normal(float v, float& e) {
   const float t = inverse(fmaf(fabsf(v), 0.3f, 1.f));
   e = exp2_(v * v * (-0.5f * kLog2e));
@@ -227,6 +228,12 @@ __device__ __forceinline__ void act_slopes(int act, const float (&p)[N], float (
   }
 }
 
+// An element as memory holds it (float, or the bits of a bf16) and as a number.
+__device__ __forceinline__ float widen(float v) { return v; }
+__device__ __forceinline__ float widen(unsigned short v) { return __uint_as_float((uint32_t)v << 16); }
+__device__ __forceinline__ void narrow(float v, float& out) { out = v; }
+__device__ __forceinline__ void narrow(float v, unsigned short& out) { out = __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
+
 __device__ __forceinline__ float epi_load(const void* m, int64_t at, int dtype) {
   return dtype == GRIM_F32 ? static_cast<const float*>(m)[at] : __bfloat162float(static_cast<const __nv_bfloat16*>(m)[at]);
 }
@@ -292,7 +299,8 @@ __device__ __forceinline__ void residual_ahead(const SpmmArgs& a, int64_t row, i
 // A warp's 32 x 32 piece of the output, left in shared memory by row with a pitch of 33 floats (bias included).  Residual, P and Y
 // go in 16-byte vectors, a warp instruction taking eight (bf16) or four (fp32) rows of 32 columns, where they are aligned and all
 // columns are there.  The residual of a piece is fetched while the piece before it is worked on (the first one while the
-// multiplies run): one trip to memory after the other cost 110 us at 8192^2 x 1024 in bf16, this, gelu included, 8.
+// multiplies run): one trip to memory after the other cost 110 us at 8192^2 x 1024 in bf16, this, bias
+// and gelu included, 8 (115.5 -> 123.5; the residual alone 2, gelu alone 2.5).
 struct PieceRes { uint4 v[8]; };
 
 // row: the output row of piece row `lane`, below 0 for none; q: the piece's first column, a multiple of 32.

@@ -19,8 +19,8 @@
 // more array, and in bf16 the difference h_{t-1} - V would be one of rounded numbers.)
 //
 // What bounds it (us; in brackets the bytes at 6.54 TB/s): fp32 decays, 2048 x 8192: 33.5 (31) forward, memory; 63 (51) backward.  bf16
-// gates, 2048 x 16384: 42 (31) and 73 (51): instructions, issued in 45 and 62 % of the cycles with the sixteen warps an SM that the
-// registers leave; the stalls are the scans' fixed latencies.  24 sequences in a row: 60 and 115, for their marks and selects.  64 rows of
+// gates, 2048 x 16384: 42 (31) and 73 (51): instructions, issued in 45 and 62 % of the cycles by the 12 to 13 warps an SM that 2048 rows of
+// a warp each make; the stalls are the scans' fixed latencies.  24 sequences in a row: 60 and 115, for their marks and selects.  64 rows of
 // 100003 columns, bf16: 19 (6) and 30 (10): rounds whose blocks wait for each other.
 #include <cuda_bf16.h>
 
@@ -51,11 +51,6 @@ struct GlrParams {
 };
 
 // ---- the columns of a lane: as memory holds them, as numbers --------------------------------------------------------
-__device__ __forceinline__ float widen(float v) { return v; }
-__device__ __forceinline__ float widen(unsigned short v) { return __uint_as_float((uint32_t)v << 16); }
-__device__ __forceinline__ void narrow(float v, float& out) { out = v; }
-__device__ __forceinline__ void narrow(float v, unsigned short& out) { out = __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
-
 // Rows need not start on 16-byte boundaries (an odd number of columns is the rule where sequences are packed).  A row's columns
 // are therefore counted in pieces that begin `shift` columns in front of it, shift being how far G's row starts behind a
 // boundary: then G's pieces lie on boundaries, and so do those of every other operand that lies like G.  For one that does not,
@@ -627,7 +622,7 @@ __device__ __forceinline__ void backward_row(const GlrParams& p, Shared& shared,
       load(rg, g_row, seg, lane, p.N);
       load(rv, v_row, seg, lane, p.N);
       if (p.dY) load(rd, d_row, seg, lane, p.N);
-      // and two rounds behind it into L2: sixteen warps with a round each in their registers do not keep the memory busy (2048 x 16384,
+      // and two rounds behind it into L2: a dozen warps with a round each in their registers do not keep the memory busy (2048 x 16384,
       // bf16: 98 -> 89 us, 24 sequences 136 -> 123; 2048 x 8192, fp32: 72 -> 66; four rounds: no better).  Forward, where a
       // round is twice as wide, it costs more than it gives (45 -> 48).
       const int far = at.columns(r - 2);
