@@ -587,7 +587,8 @@ __device__ __forceinline__ void forward_row(const GlrParams& p, Shared& shared, 
 }
 
 // (registers: what lets a block of one warp per row, or the blocks of two warps with L = 8, stay on the SM all at once, sixteen or 28
-// warps; a few more or less spill or push the last rows into a second round: 128 and 72 were the best of 64 to 168)
+// warps; with sixteen columns 12 to 40 bytes of a thread are spilled at 128.  Fewer spill more, more push the last rows into a second round: 128 and
+// 72 were the best of 64 to 168)
 template <bool PACKED, typename TI, typename TO, int L>
 __global__ void __maxnreg__(L == 8 ? 72 : 128) glr_forward_kernel(const __grid_constant__ GlrParams p) {
   extern __shared__ uint32_t dynamic[];
